@@ -767,14 +767,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) q4_join_kernel(const Q4Decode
 #pragma unroll 4
     for (int i = warp % W; i < jn.z; i += W) {
       const float* p = part(i);
+      // (parts without a row are zeros; a NaN shows whatever its part's weight)
       const float m = p[D], f = m == -INFINITY ? 0.f : fast_exp2(m - M);
-      const float l = p[D + 1];
-      L += f == 0.f ? 0.f : f * l;
+      L += f * p[D + 1];
 #pragma unroll
-      for (int k = 0; k < E; ++k) {
-        const float v = p[lane + 32 * k];
-        o[k] += f == 0.f ? 0.f : f * v;
-      }
+      for (int k = 0; k < E; ++k) o[k] += f * p[lane + 32 * k];
     }
   }
 #pragma unroll

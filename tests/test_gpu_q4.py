@@ -883,3 +883,41 @@ def test_single_rows_of_large_batches(L, b, Hkv, d):
                     c.write(s, l, h, pos[s] + j, k64[l, s, h, max(i, 0)], v64[l, s, h, max(i, 0)], i < 0)
     c.check_pool()
     assert st.item() == 0
+
+
+def sms():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+@pytest.mark.parametrize("seqs", [1, 120])
+@pytest.mark.parametrize("where", ["keys", "values"])
+def test_a_part_of_no_weight_keeps_its_nan(seqs, where):
+    """Rows of a sequence shared by several CTAs: NaN keys that fill a CTA's part,
+    and a NaN value in a part whose logits lie hundreds below the others', show in
+    the outputs as they do where one CTA has all rows.  Units begin with 32 to
+    256 such rows, so that some of them fill a part and no more."""
+    d, P, G, n = 64, 64, 2, 2048 if seqs == 1 else 900
+    Hkv = 8 if seqs == 1 else 1
+    units = seqs * Hkv
+    assert (4 * units <= 3 * sms()) == (seqs == 1)            # joined by unit, or by the CTA that begins one
+    lens = [n] * seqs
+    c = Cache(seqs, pages_for(lens, P), P, -(-n // P), 1, Hkv, d).fill(lens, shuffle=2)
+    k, v = torch.full((1, seqs, Hkv, n, d), 8.0), bf16((1, seqs, Hkv, n, d), 2).float()
+    first = torch.tensor([32 * (1 + (u // 8 if seqs > 1 else u) % 8) for u in range(units)]).view(seqs, Hkv)
+    for s in range(seqs):
+        for h in range(Hkv):
+            if where == "keys":
+                k[0, s, h, :first[s, h]] = float("nan")
+            else:
+                k[0, s, h, :first[s, h]] = 0.0
+                v[0, s, h, 5, 3] = float("nan")
+    R.kv_append_q4(c.pool, c.pages, k.bfloat16().to(DEV), v.bfloat16().to(DEV), i32([0] * seqs))
+    q = torch.full((1, seqs, Hkv * G, d), 8.0).bfloat16()
+    out = torch.empty(q.shape, device=DEV)
+    R.decode_attention_q4(q.to(DEV), c.pool, c.pages, out)
+    got = out.cpu()
+    if where == "keys":
+        assert torch.isnan(got).all(), f"{int(torch.isfinite(got).any(-1).sum())} heads of {got.shape[2] * seqs} are finite"
+    else:
+        assert torch.isnan(got[..., :32]).all(), "a NaN value does not show"
+        assert torch.isfinite(got[..., 32:]).all()
