@@ -482,7 +482,7 @@ int kv_expand_q4(const rolekv_pool* pool, const rolekv_pages* pages, const int32
  * are the same bits for the same lengths.  Sums, softmax statistics and outputs
  * are fp32; a probability times its row's V scale counts with 22 bits, down to
  * 2^-34 of the largest.  A NaN, or a query that is not finite, gives NaN in the
- * outputs that it reaches; values beyond 2^100 lose small probabilities. */
+ * outputs that it reaches. */
 int rolekv_decode_q4_workspace_size(int32_t L, int32_t b, int32_t Hq, int32_t Hkv, int32_t d, size_t* bytes);
 int decode_attention_q4(const rolekv_pool* pool, const rolekv_pages* pages, const int32_t* seqs, int32_t b, int32_t Hq,
                         rolekv_tensor q, float scale, float* out, void* workspace, size_t workspace_bytes,

@@ -28,9 +28,13 @@
 //   O = V^T P   16 elements x heads over 16 rows.  The probabilities change
 //     places through shared memory; a row's times its V scale is a lane's own
 //     value.  It goes in as two fp16 numbers, the upper bits and the rest, so
-//     that 22 bits count.  A power of two in the softmax's reference keeps them
-//     below 2^15 whatever the scales, and the largest above 2^10, so that
-//     fp16's smallest step is 2^-34 of the largest at most.
+//     that 22 bits count.  The probabilities are taken times a power of two, by
+//     the largest V scale so far, which keeps the numbers below 2^15 and the
+//     largest above 2^10, so that fp16's smallest step is 2^-34 of the largest at
+//     most.  The power is no part of the softmax's reference (which would save
+//     the product, 1% of the time): beside large logits fp32 has no room for it,
+//     and the probabilities' sums would span more powers of two than fp32 has.
+//     A warp's sums leave it as means, the power taken off.
 // What bounds it is instructions: some 390 a record and warp, of which about 145
 // make operands of codes, issued 0.6 a cycle and scheduler with the ALU pipe at
 // 46%, FMA 39%, tensor 30%, DRAM 49%.  131072 rows of 8 heads, 151 MB: 45 us,
@@ -42,6 +46,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -59,6 +64,7 @@ constexpr int kHeads = 8;           // columns of the products: query heads of a
 constexpr int kRecs = 2;            // records of a piece
 constexpr int kPieceRows = kRecs * kQ4Rows;
 constexpr int kSlack = 4;           // powers of two a logit may pass the largest so far by before the sums are rescaled
+constexpr int kMaxRoom = 96;        // of the power of two that probabilities are taken times
 constexpr int kTurn = 12;           // floats of a row of probabilities (eight, and room against bank conflicts)
 
 // How the rows are shared: an even run of pieces to each CTA, with what is to
@@ -140,6 +146,13 @@ __device__ __forceinline__ uint32_t low_codes(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) {
   return add_half2(and_or(w, 0x00F000F0u, 0x64006400u), 0xE480E480u);   // -1152
+}
+
+// 1 / x, off by 2^-23 of it.
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
@@ -468,9 +481,11 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
         qb[j][3] = pack_half2(e[3] * 0.0625f, e[7] * 0.0625f);
       }
     }
-    // heads 2t and 2t + 1: what a logit may reach, reference, sum over this lane's rows
-    float top[2] = {-INFINITY, -INFINITY}, ref[2] = {0.f, 0.f}, den[2] = {0.f, 0.f};
+    // heads 2t and 2t + 1: reference (a logit, kSlack below the largest at most),
+    // sum over this lane's rows
+    float ref[2] = {-FLT_MAX, -FLT_MAX}, den[2] = {0.f, 0.f};
     uint32_t top_scale = 0;                         // what a V scale may reach (bf16 bits, twice; all lanes)
+    float room = pow2(kMaxRoom);                    // the power of two that probabilities are taken times
     float acc[2 * J][4];
 #pragma unroll
     for (int i = 0; i < 2 * J; ++i)
@@ -547,11 +562,11 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
         }
       const float m0 = fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2]));
       const float m1 = fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]));
-      if (__any_sync(0xffffffffu, m0 > top[0] || m1 > top[1] || sc != top_scale)) {
-        // A logit well above the largest so far, or a V scale of a new power of
-        // two: the reference moves up (rarely, once a unit is under way).  It is
-        // the largest logit less `room`, so that probability * scale stays
-        // below 2^15 while logits pass that one by kSlack at most.
+      if (__any_sync(0xffffffffu, m0 - ref[0] > kSlack || m1 - ref[1] > kSlack || sc != top_scale)) {
+        // A logit well above the reference, or a V scale of a new power of two:
+        // the reference moves up to the largest logit, and the power that
+        // probabilities are taken times down (rarely, once a unit is under way),
+        // so that probability * scale stays below 2^15.
         uint32_t big = top_scale & 0xFFFFu;
 #pragma unroll
         for (int r = 0; r < kRecs; ++r)
@@ -565,20 +580,21 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
             }
         big = __reduce_max_sync(0xffffffffu, big) | 0x7Fu;
         top_scale = big | (big << 16);
-        const int e = 141 - kSlack - static_cast<int>(big >> 7);
-        const float room = static_cast<float>(e < 96 ? e : 96);
+        const int e = 141 - kSlack - static_cast<int>(big >> 7) + 127, fit = min(e, kMaxRoom + 127);
+        // (a step of more than 2^-126 leaves sums too large, but far below a new term)
+        const float shrink = pow2(max(fit - static_cast<int>(__float_as_uint(room) >> 23), -126));
+        room = __uint_as_float(static_cast<uint32_t>(fit) << 23);
         float f[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float mx = i == 0 ? m0 : m1;
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-          mx = fmaxf(mx, top[i] - kSlack);
-          const float to = mx == -INFINITY ? 0.f : mx - room;
-          f[i] = top[i] == -INFINITY ? 1.f : fast_exp2(ref[i] - to);
-          top[i] = mx + kSlack;
-          ref[i] = to;
+          mx = fmaxf(mx, ref[i]);
+          f[i] = fast_exp2(ref[i] - mx);
+          ref[i] = mx;
           den[i] *= f[i];
+          f[i] *= shrink;
         }
 #pragma unroll
         for (int i = 0; i < 2 * J; ++i) {
@@ -592,11 +608,13 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
 #pragma unroll
       for (int r = 0; r < kRecs; ++r) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[r][i] = fast_exp2(x[r][i] - ref[i & 1]);
-        den[0] += x[r][0] + x[r][2];
-        den[1] += x[r][1] + x[r][3];
-        *reinterpret_cast<float2*>(turn_to + r * kQ4Rows * kTurn) = make_float2(x[r][0], x[r][1]);
-        *reinterpret_cast<float2*>(turn_to + (r * kQ4Rows + 8) * kTurn) = make_float2(x[r][2], x[r][3]);
+        for (int hf = 0; hf < 2; ++hf) {
+          const float2 y = __fadd2_rn(make_float2(x[r][2 * hf], x[r][2 * hf + 1]), make_float2(-ref[0], -ref[1]));
+          const float2 p = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+          den[0] += p.x;
+          den[1] += p.y;
+          *reinterpret_cast<float2*>(turn_to + (r * kQ4Rows + 8 * hf) * kTurn) = __fmul2_rn(p, make_float2(room, room));
+        }
       }
       __syncwarp();
       // ----------------------------------------------------------- values --
@@ -659,12 +677,15 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
     }
 
     // ------------------------------------------------- the unit (part) ends --
+    // (the means over the warp's rows, whose size is the values' own: a sum, or
+    // one with the power of two still on, may lie outside fp32)
+    float mean[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) den[i] += __shfl_xor_sync(0xffffffffu, den[i], o);
-      if (g == 0)
-        stat[warp][2 * t + i] = make_float2(top[i] == -INFINITY && den[i] == 0.f ? -INFINITY : ref[i], den[i]);
+      mean[i] = den[i] == 0.f ? 0.f : pow2(127 - static_cast<int>(__float_as_uint(room) >> 23)) * reciprocal(den[i]);
+      if (g == 0) stat[warp][2 * t + i] = make_float2(den[i] == 0.f ? -INFINITY : ref[i], den[i]);
     }
     const Work w = work;
     const bool whole = w.unit.start >= x0 && w.unit.end <= x1;
@@ -681,26 +702,28 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const float *c = acc[2 * j], *d = acc[2 * j + 1];
-          *reinterpret_cast<float4*>(y + 32 * j) = make_float4(c[0], c[2] * 0.0625f, d[0], d[2] * 0.0625f);
-          *reinterpret_cast<float4*>(y + HEAD + 32 * j) = make_float4(c[1], c[3] * 0.0625f, d[1], d[3] * 0.0625f);
+          const float m0 = mean[0], m1 = mean[1], n0 = m0 * 0.0625f, n1 = m1 * 0.0625f;
+          *reinterpret_cast<float4*>(y + 32 * j) = make_float4(c[0] * m0, c[2] * n0, d[0] * m0, d[2] * n0);
+          *reinterpret_cast<float4*>(y + HEAD + 32 * j) = make_float4(c[1] * m1, c[3] * n1, d[1] * m1, d[3] * n1);
         }
       }
       sync_consumers();
       for (int i = threadIdx.x; i < 4 * D && h0 + i / D < G && write; i += kThreads) {
         const int hd = h0 + i / D, e = i % D;
-        float M = -INFINITY, L = 0.f, o = 0.f;
+        float M = -INFINITY, L = 0.f, o = 0.f, part_of[kWarps];
 #pragma unroll
         for (int x = 0; x < kWarps; ++x) M = fmaxf(M, stat[x][hd].x);
 #pragma unroll
         for (int x = 0; x < kWarps; ++x) {
           const float2 st = stat[x][hd];
-          if (st.x == -INFINITY) continue;
-          const float f = fast_exp2(st.x - M);
-          L += f * st.y;
-          o += f * sums[(x * 4 + i / D) * HEAD + e];
+          part_of[x] = st.x == -INFINITY ? 0.f : fast_exp2(st.x - M) * st.y;
+          L += part_of[x];
         }
+        const float by_all = L == 0.f ? 0.f : reciprocal(L);
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) o += part_of[x] * by_all * sums[(x * 4 + i / D) * HEAD + e];
         if (whole) {
-          a.out[out + hd * D + e] = L == 0.f ? 0.f : o / L;
+          a.out[out + hd * D + e] = o;
         } else {
           float* y = a.part + part + hd * (D + 2);
           y[e] = o;
@@ -746,7 +769,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) q4_join_kernel(const Q4Decode
   constexpr int E = D / 32;
   constexpr int H = kFew ? 1 : kHeads;              // heads of a CTA
   constexpr int W = kJoinWarps / H;                 // warps of a head
-  __shared__ float sums[kJoinWarps][D + 1];
+  __shared__ float sums[kJoinWarps][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.G, item = kFew ? blockIdx.x / G : blockIdx.x, h0 = kFew ? blockIdx.x % G : 0;
   wait_for_previous_kernels();
@@ -756,40 +779,46 @@ __global__ void __launch_bounds__(kJoinWarps * 32) q4_join_kernel(const Q4Decode
   const auto part = [&](int i) {
     return a.part + static_cast<int64_t>(i == 0 ? jn.y : 2 * (first_cta + i)) * G * (D + 2) + hd * (D + 2);
   };
-  float o[E], L = 0.f;
+  float o[E];
 #pragma unroll
   for (int k = 0; k < E; ++k) o[k] = 0.f;
   if (hd < G) {
-    float M = -INFINITY;
-    for (int i = lane; i < jn.z; i += 32) M = fmaxf(M, part(i)[D]);
+    // the parts' largest reference and, by it, the sum of all probabilities
+    float M = -INFINITY, L = 0.f;
+    const auto add = [&](float m, float l) {
+      const float to = fmaxf(M, m);
+      if (to == -INFINITY) return;
+      L = L * fast_exp2(M - to) + l * fast_exp2(m - to);
+      M = to;
+    };
+    for (int i = lane; i < jn.z; i += 32) add(part(i)[D], part(i)[D + 1]);
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+    for (int x = 16; x > 0; x >>= 1) {
+      const float m = __shfl_xor_sync(0xffffffffu, M, x), l = __shfl_xor_sync(0xffffffffu, L, x);
+      add(m, l);
+    }
+    const float by_all = L == 0.f ? 0.f : reciprocal(L);
 #pragma unroll 4
     for (int i = warp % W; i < jn.z; i += W) {
       const float* p = part(i);
       // (parts without a row are zeros; a NaN shows whatever its part's weight)
-      const float m = p[D], f = m == -INFINITY ? 0.f : fast_exp2(m - M);
-      L += f * p[D + 1];
+      const float f = p[D] == -INFINITY ? 0.f : fast_exp2(p[D] - M) * p[D + 1] * by_all;
 #pragma unroll
       for (int k = 0; k < E; ++k) o[k] += f * p[lane + 32 * k];
     }
   }
 #pragma unroll
   for (int k = 0; k < E; ++k) sums[warp][lane + 32 * k] = o[k];
-  if (lane == 0) sums[warp][D] = L;
   __syncthreads();
   const int64_t out = (static_cast<int64_t>(jn.x) * G + h0) * D;
   const int heads = kFew ? 1 : G;
   if (!in_bounds(out, heads * D, a.ext_out, a.p.status)) return;
   for (int i = threadIdx.x; i < heads * D; i += kJoinWarps * 32) {
     const int h = i / D, e = i % D;
-    float v = 0.f, z = 0.f;
+    float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      v += sums[h * W + w][e];
-      z += sums[h * W + w][D];
-    }
-    a.out[out + i] = z == 0.f ? 0.f : v / z;
+    for (int w = 0; w < W; ++w) v += sums[h * W + w][e];
+    a.out[out + i] = v;
   }
 }
 

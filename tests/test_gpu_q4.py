@@ -921,3 +921,44 @@ def test_a_part_of_no_weight_keeps_its_nan(seqs, where):
     else:
         assert torch.isnan(got[..., :32]).all(), "a NaN value does not show"
         assert torch.isfinite(got[..., 32:]).all()
+
+
+@pytest.mark.parametrize("n", [384, 4000])
+@pytest.mark.parametrize("before, after", [(0.0, 2.0 ** 45), (2.0 ** -60, 2.0 ** 60), (2.0 ** 45, 0.0),
+                                           (2.0 ** 99, 2.0 ** -99), (2.0 ** -99, 2.0 ** 99), (0.0, 2.0 ** 124)])
+def test_attention_over_values_that_change_in_size(n, before, after):
+    """Rows of values of one size, then as many of another: all count with the
+    weights that their keys give them, in one CTA and over several."""
+    d, G, P = 64, 2, 32
+    c = Cache(1, pages_for([n], P), P, -(-n // P), 1, 1, d).fill([n], shuffle=1)
+    v = bf16((1, 1, 1, n, d), 4).double().clamp(-3, 3)
+    v[..., :n // 2, :] *= before
+    v[..., n // 2:, :] *= after
+    R.kv_append_q4(c.pool, c.pages, bf16((1, 1, 1, n, d), 3).to(DEV), v.bfloat16().to(DEV), i32([0]))
+    c.want = c.pool.cpu().numpy()
+    q = bf16((1, 1, G, d), 9)
+    out = torch.empty((1, 1, G, d), device=DEV)
+    R.decode_attention_q4(q.to(DEV), c.pool, c.pages, out)
+    check_attention(out, q, c)
+
+
+@pytest.mark.parametrize("n", [300, 4000])
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 16, 2.0 ** 40])
+@pytest.mark.parametrize("scale", [20.0, 2.0 ** 30])
+def test_attention_of_large_equal_logits(n, size, scale):
+    """Keys that are all the same, with logits of 2^27 and more, whose steps in
+    fp32 are larger than any exponent of two that the values' size asks for: the
+    mean of the values.  Equal logits give equal probabilities, so an output is
+    off by n rounded additions and, 22 bits of each product, 2^-21 of mean |v|."""
+    d, G, P = 128, 3, 32
+    c = Cache(1, pages_for([n], P), P, -(-n // P), 1, 1, d).fill([n], shuffle=1)
+    k = torch.full((1, 1, 1, n, d), 2896.0 * size / 4096)
+    v = bf16((1, 1, 1, n, d), 4).clamp(-1, 1) * scale
+    R.kv_append_q4(c.pool, c.pages, k.bfloat16().to(DEV), v.to(DEV), i32([0]))
+    c.want = c.pool.cpu().numpy()
+    q = torch.full((1, 1, G, d), size).bfloat16()
+    out = torch.empty((1, 1, G, d), device=DEV)
+    R.decode_attention_q4(q.to(DEV), c.pool, c.pages, out)
+    v64 = c.rows(0, 0, 0)[1]
+    tol = ((n + 64) * 2.0 ** -24 + 2.0 ** -20) * np.abs(v64).mean(0)
+    assert (np.abs(f64(out)[0, 0] - v64.mean(0)) <= tol).all()
