@@ -482,7 +482,9 @@ int kv_expand_q4(const rolekv_pool* pool, const rolekv_pages* pages, const int32
  * are the same bits for the same lengths.  Sums, softmax statistics and outputs
  * are fp32; a probability times its row's V scale counts with 22 bits, down to
  * 2^-34 of the largest.  A NaN, or a query that is not finite, gives NaN in the
- * outputs that it reaches. */
+ * outputs that it reaches.  Keys are below 2^105 in magnitude: larger ones may
+ * give NaN where the logits themselves are finite (queries and values may be any
+ * that bf16 holds). */
 int rolekv_decode_q4_workspace_size(int32_t L, int32_t b, int32_t Hq, int32_t Hkv, int32_t d, size_t* bytes);
 int decode_attention_q4(const rolekv_pool* pool, const rolekv_pages* pages, const int32_t* seqs, int32_t b, int32_t Hq,
                         rolekv_tensor q, float scale, float* out, void* workspace, size_t workspace_bytes,

@@ -22,9 +22,11 @@
 //   S = K Q^T   16 rows x heads.  q is scaled by a power of two to below 2^15,
 //     and then is exact in fp16 (elements below 2^-25 of a head's largest lose
 //     bits, 2^-39 of it at most), and by 2^-4 where codes come times 16.  Each
-//     group's sum is scaled in fp32.  (As Q K^T the logits would come out in
-//     the layout that the next product wants, but half of its rows, and of the
-//     registers that hold q, would be zeros.)
+//     group's sum is scaled in fp32, q's power of two still on: a row's sum stays
+//     below 7 * 128 * 2^15 scales, within fp32 for scales below 2^103, keys below
+//     2^105.  (As Q K^T the logits would come out in the layout that the next
+//     product wants, but half of its rows, and of the registers that hold q,
+//     would be zeros.)
 //   O = V^T P   16 elements x heads over 16 rows.  The probabilities change
 //     places through shared memory; a row's times its V scale is a lane's own
 //     value.  It goes in as two fp16 numbers, the upper bits and the rest, so

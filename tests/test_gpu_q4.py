@@ -962,3 +962,30 @@ def test_attention_of_large_equal_logits(n, size, scale):
     v64 = c.rows(0, 0, 0)[1]
     tol = ((n + 64) * 2.0 ** -24 + 2.0 ** -20) * np.abs(v64).mean(0)
     assert (np.abs(f64(out)[0, 0] - v64.mean(0)) <= tol).all()
+
+
+@pytest.mark.parametrize("n", [130, 2000])
+@pytest.mark.parametrize("q0, k0", [(1.0, 2.0 ** 104), (2.0 ** -20, 2.0 ** 104), (2.0 ** 20, 2.0 ** 98),
+                                    (2.0 ** 100, 2.0 ** 18), (2.0 ** 127, 2.0 ** -9)])
+def test_attention_of_the_largest_keys_and_queries(n, q0, k0):
+    """Keys up to the header's limit, and queries up to bf16's, of logits up to
+    2^122: the row of the largest has all the weight.  d 128, so that all four
+    groups add up."""
+    d, P = 128, 32
+    c = Cache(1, pages_for([n], P), P, -(-n // P), 1, 1, d).fill([n], shuffle=1)
+    k = torch.full((1, 1, 1, n, d), k0)
+    best = n // 3
+    k[..., best, :] *= 1.5
+    k[..., ::5, :] *= -1.0
+    k[..., best, :] = k[..., best, :].abs()
+    R.kv_append_q4(c.pool, c.pages, k.bfloat16().to(DEV), bf16((1, 1, 1, n, d), 4).to(DEV), i32([0]))
+    c.want = c.pool.cpu().numpy()
+    q = torch.full((1, 1, 3, d), q0)
+    q[0, 0, 1] *= -1.0                                        # (the rows of the least: equal logits, not checked)
+    q[0, 0, 2] = 0.0
+    out = torch.empty((1, 1, 3, d), device=DEV)
+    R.decode_attention_q4(q.bfloat16().to(DEV), c.pool, c.pages, out)
+    got, v = f64(out)[0, 0], c.rows(0, 0, 0)[1]
+    assert np.isfinite(got).all()
+    assert (np.abs(got[0] - v[best]) <= 2.0 ** -20 * np.abs(v[best])).all()
+    assert (np.abs(got[2] - v.mean(0)) <= ((n + 64) * 2.0 ** -24 + 2.0 ** -20) * np.abs(v).mean(0)).all()
