@@ -466,7 +466,10 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
       m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
       int k = 14 + 127 - static_cast<int>(m >> 7);  // largest element in [2^14, 2^15)
       k = k > 126 ? 126 : k;
-      const float up = pow2(k), logit = a.c1 * pow2(-k);
+      // (a query that is not finite reaches the rows that there are, and gives NaN
+      // if there are any: it is taken as zeros and marked by the sign)
+      const bool finite = m < 0x7F80u;
+      const float up = pow2(k), logit = finite ? a.c1 * pow2(-k) : -0.f;
       logit0 = __shfl_sync(0xffffffffu, logit, 8 * t);
       logit1 = __shfl_sync(0xffffffffu, logit, 8 * t + 4);
 #pragma unroll
@@ -474,6 +477,7 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
         float e[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+          if (!finite) raw[j][i] = 0u;
           e[2 * i] = __uint_as_float(raw[j][i] << 16) * up;
           e[2 * i + 1] = __uint_as_float(raw[j][i] & 0xFFFF0000u) * up;
         }
@@ -686,6 +690,7 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) den[i] += __shfl_xor_sync(0xffffffffu, den[i], o);
+      if (signbit(i == 0 ? logit0 : logit1) && den[i] != 0.f) den[i] = NAN;
       mean[i] = den[i] == 0.f ? 0.f : pow2(127 - static_cast<int>(__float_as_uint(room) >> 23)) * reciprocal(den[i]);
       if (g == 0) stat[warp][2 * t + i] = make_float2(den[i] == 0.f ? -INFINITY : ref[i], den[i]);
     }

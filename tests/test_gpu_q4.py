@@ -989,3 +989,32 @@ def test_attention_of_the_largest_keys_and_queries(n, q0, k0):
     assert np.isfinite(got).all()
     assert (np.abs(got[0] - v[best]) <= 2.0 ** -20 * np.abs(v[best])).all()
     assert (np.abs(got[2] - v.mean(0)) <= ((n + 64) * 2.0 ** -24 + 2.0 ** -20) * np.abs(v).mean(0)).all()
+
+
+@pytest.mark.parametrize("n", [40, 1000])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_query_that_is_not_finite_over_empty_slots(n, bad):
+    """It reaches no row of a sequence of empty slots, whose outputs are zeros;
+    where there are rows it gives NaN, and the other heads keep their outputs."""
+    d, P, G = 64, 16, 3
+    lens = [n, n, 0, n]
+    c = Cache(4, pages_for(lens, P), P, -(-n // P), 1, 1, d).fill(lens, shuffle=1)
+    batch = R.Batch(1, 4, G, 1, d, n)
+    k, v = bf16((1, 4, 1, n, d), 1).to(DEV), bf16((1, 4, 1, n, d), 2).to(DEV)
+    idx = torch.arange(n, dtype=torch.int32).repeat(4, 1).view(1, 4, 1, n)
+    idx[:, 1] = -1
+    idx[:, 3, :, 3:] = -1
+    R.kv_compact_q4(batch, k, v, idx.to(DEV), 1.0, c.pool, c.pages, i32([0, 0, -1, 0]))
+    c.want = c.pool.cpu().numpy()
+    q = bf16((1, 4, G, d), 9)
+    q[:, :, 1, 5] = bad
+    out = torch.full((1, 4, G, d), 7.0, device=DEV)
+    R.decode_attention_q4(q.to(DEV), c.pool, c.pages, out)
+    got = out.cpu()
+    assert torch.isnan(got[0, 0, 1]).all() and torch.isnan(got[0, 3, 1]).all()
+    assert (got[0, 1:3] == 0).all()
+    q[:, :, 1, 5] = 0
+    want = torch.empty_like(out)
+    R.decode_attention_q4(q.to(DEV), c.pool, c.pages, want)
+    out[:, :, 1] = want[:, :, 1]
+    check_attention(out, q, c)
