@@ -445,8 +445,9 @@ int kv_pages_pack(const rolekv_pages* pages, const rolekv_pool* pool, int32_t* n
  * and budget as for kv_compact; index -1: an empty slot).  pos (device int32
  * [n_seqs]) is what kv_pages_reserve gave; -1: nothing is written.  The pool
  * holds the batch's layers and heads.  Rows before and behind these are left
- * as they are.  (The rows of a reserve are on pages of the slot's own; rows
- * written elsewhere change for every slot that holds their page.) */
+ * as they are.  As for kv_compact, k and v may point into pinned host memory.
+ * (The rows of a reserve are on pages of the slot's own; rows written elsewhere
+ * change for every slot that holds their page.) */
 int kv_compact_q4(const rolekv_batch* batch, rolekv_tensor k, rolekv_tensor v, const int32_t* keep_idx, float budget,
                   const rolekv_pool* pool, const rolekv_pages* pages, const int32_t* seqs, const int32_t* pos,
                   int32_t* status_dev, void* stream);

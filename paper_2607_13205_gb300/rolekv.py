@@ -550,8 +550,13 @@ def kv_pages_pack(pages: Pages, pool: torch.Tensor, n_live: Optional[torch.Tenso
 def kv_compact_q4(batch: Batch, k: torch.Tensor, v: torch.Tensor, keep_idx: torch.Tensor, budget: float,
                   pool: torch.Tensor, pages: Pages, pos: torch.Tensor, seqs: Optional[torch.Tensor] = None,
                   status: Optional[torch.Tensor] = None, stream=None):
-    """The kept rows of K and V into rows pos[x] .. of the cache."""
-    st = _here(stream, pages.state, pool, k, v, keep_idx, pos, seqs, status, batch.cu_seqlens)
+    """The kept rows of K and V into rows pos[x] .. of the cache.  K and V may
+    lie in pinned host memory, of which the kept rows alone are read."""
+    st = _here(stream, pages.state, pool, keep_idx, pos, seqs, status, batch.cu_seqlens)
+    dev = pool.get_device()
+    for t in (k, v):
+        if t.get_device() != dev and not (t.device.type == "cpu" and t.is_pinned()):
+            raise ValueError(f"k or v on {t.device}: neither on the current device, cuda:{dev}, nor in pinned host memory")
     _check(lib().kv_compact_q4(ctypes.byref(batch.desc), _rows_desc(batch, k, "k"), _rows_desc(batch, v, "v"),
                                _int32(keep_idx, batch.L * batch.Hkv * max(0, batch.kept_total(budget)), "keep_idx"),
                                budget, ctypes.byref(pool_desc(pool, pages)),

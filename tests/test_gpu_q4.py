@@ -1018,3 +1018,35 @@ def test_a_query_that_is_not_finite_over_empty_slots(n, bad):
     R.decode_attention_q4(q.to(DEV), c.pool, c.pages, want)
     out[:, :, 1] = want[:, :, 1]
     check_attention(out, q, c)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("budget", [0.1, 0.9])
+def test_compact_from_pinned_host_memory(budget, packed):
+    """K and V left in pinned host memory, a few rows and whole records: the
+    bytes that the same rows on the device give."""
+    L, b, Hkv, n, d, P = 2, 2, 2, 40, 128, 16
+    shape = (L, b * n, Hkv, d) if packed else (L, b, Hkv, n, d)
+    k, v = bf16(shape, 1), bf16(shape, 2)
+    batch = R.Batch(L, b, Hkv, Hkv, d, n, seqlens=[n, n] if packed else None)
+    m = R.kept_rows(n, budget)
+    idx = torch.sort(torch.rand((L, b, Hkv, n), generator=torch.Generator().manual_seed(3)).topk(m).indices).values
+    idx = idx.permute(0, 2, 1, 3).reshape(L, Hkv, b * m) if packed else idx
+    lens = [m + 3] * b
+    pools = []
+    for where in ("device", "host", "one each"):
+        c = Cache(b, pages_for(lens, P), P, 4, L, Hkv, d, seed=1).fill(lens, shuffle=1)
+        kk = k.to(DEV) if where == "device" else k.pin_memory()
+        vv = v.pin_memory() if where == "host" else v.to(DEV)
+        st = new_status()
+        R.kv_compact_q4(batch, kk, vv, idx.int().contiguous().to(DEV), budget, c.pool, c.pages, i32([3] * b), status=st)
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        pools.append(c.pool.cpu())
+    assert torch.equal(pools[0], pools[1]) and torch.equal(pools[0], pools[2])
+    for kk, vv in ((k, v.to(DEV)), (k.to(DEV), v), (k, v)):
+        with pytest.raises(ValueError, match="pinned"):
+            R.kv_compact_q4(batch, kk, vv, idx.int().contiguous().to(DEV), budget, c.pool, c.pages, i32([3] * b))
+    with pytest.raises(ValueError, match="current device"):
+        R.kv_append_q4(c.pool, c.pages, bf16((L, b, Hkv, 1, d), 1).pin_memory(), bf16((L, b, Hkv, 1, d), 2).to(DEV),
+                       i32([3] * b))
