@@ -462,7 +462,7 @@ int kv_append_q4(const rolekv_pool* pool, const rolekv_pages* pages, const int32
 /* Rows read back as bf16 (a second round of scoring reads them so): row
  * start[x] + j of sequence s's slot x (start NULL: 0) goes to row j of k_out
  * and v_out, bf16 [L][b][Hkv][rows][d] by strides, for every j < rows that the
- * slot holds; the others are left as they are.  Values are rounded to bf16 to
+ * slot holds on a page; the others are left as they are.  Values are rounded to bf16 to
  * nearest, ties to even. */
 int kv_expand_q4(const rolekv_pool* pool, const rolekv_pages* pages, const int32_t* seqs, int32_t b,
                  const int32_t* start, int32_t rows, rolekv_tensor k_out, rolekv_tensor v_out, int32_t* status_dev,

@@ -65,15 +65,15 @@ __device__ __forceinline__ void store_words(uint8_t* p, const uint32_t* w) {
 }
 
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p, bool there) {
+__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
   if constexpr (N == 4) {
-    const uint4 x = there ? load_stream(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+    const uint4 x = load_stream(reinterpret_cast<const uint4*>(p));
     w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
   } else if constexpr (N == 2) {
-    const uint2 x = there ? load_stream(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+    const uint2 x = load_stream(reinterpret_cast<const uint2*>(p));
     w[0] = x.x, w[1] = x.y;
   } else {
-    w[0] = there ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   }
 }
 
@@ -468,17 +468,19 @@ __global__ void __launch_bounds__(kThreads) q4_expand_kernel(const Q4ExpandArgs 
   const int first = rec * kQ4Rows - start;          // output row of the record's row 0
   if (first >= rows) return;
   const int64_t at = q4_record(a.p, slot, l, h, rec);
-  bool there = at >= 0;
-  if (!there && a.p.status != nullptr && lane == 0) atomicOr(a.p.status, ROLEKV_STATUS_BAD_INDEX);
-  there = there && in_bounds(at, q4_record_bytes(D), a.p.ext_pool, a.p.status);
-  const uint8_t* const p = a.p.pool + (there ? at : 0);
+  if (at < 0) {                                     // rows that are absent: nothing to give back
+    if (a.p.status != nullptr && lane == 0) atomicOr(a.p.status, ROLEKV_STATUS_BAD_INDEX);
+    return;
+  }
+  if (!in_bounds(at, q4_record_bytes(D), a.p.ext_pool, a.p.status)) return;
+  const uint8_t* const p = a.p.pool + at;
   uint32_t kw[2][J], vw[2][J], ksc[2][J / 2], vsc[2][J];
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
-    load_words<J>(kw[hf], p + hf * 4 * D + lane * 4 * J, there);
-    load_words<J>(vw[hf], p + q4_v_codes(D) + hf * 4 * D + lane * 4 * J, there);
-    load_words<J / 2>(ksc[hf], p + q4_k_scales(D) + q4_scale(D, hf * 8 + g, 0), there);
-    load_words<J>(vsc[hf], p + q4_v_scales(D) + q4_scale(D, hf * 8 + 2 * t, 0), there);
+    load_words<J>(kw[hf], p + hf * 4 * D + lane * 4 * J);
+    load_words<J>(vw[hf], p + q4_v_codes(D) + hf * 4 * D + lane * 4 * J);
+    load_words<J / 2>(ksc[hf], p + q4_k_scales(D) + q4_scale(D, hf * 8 + g, 0));
+    load_words<J>(vsc[hf], p + q4_v_scales(D) + q4_scale(D, hf * 8 + 2 * t, 0));
   }
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(kThreads) q4_expand_kernel(const Q4ExpandArgs 
         const uint32_t sc = __byte_perm(ksc[hf][j / 2] & 0x7FFF7FFFu, 0, (j & 1) ? 0x3232 : 0x1010);
         uint32_t r[4];                              // elements i and i + 4
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = there ? two_values(kw[hf][j] >> (4 * i), sc) : 0u;
+        for (int i = 0; i < 4; ++i) r[i] = two_values(kw[hf][j] >> (4 * i), sc);
         *reinterpret_cast<uint4*>(a.k + ko + 32 * j) =
             make_uint4(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410),
                        __byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632));
@@ -502,7 +504,7 @@ __global__ void __launch_bounds__(kThreads) q4_expand_kernel(const Q4ExpandArgs 
       const uint32_t sc = __byte_perm(vsc[hf][j / 2], vsc[hf][J / 2 + j / 2], (j & 1) ? 0x7632 : 0x5410);
       uint32_t r[4];                                // element i of both rows
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = there ? two_values(vw[hf][j] >> (4 * i), sc) : 0u;
+      for (int i = 0; i < 4; ++i) r[i] = two_values(vw[hf][j] >> (4 * i), sc);
       out[0][j] = make_uint2(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410));
       out[1][j] = make_uint2(__byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632));
     }

@@ -1050,3 +1050,21 @@ def test_compact_from_pinned_host_memory(budget, packed):
     with pytest.raises(ValueError, match="current device"):
         R.kv_append_q4(c.pool, c.pages, bf16((L, b, Hkv, 1, d), 1).pin_memory(), bf16((L, b, Hkv, 1, d), 2).to(DEV),
                        i32([3] * b))
+
+
+@pytest.mark.parametrize("entry", [-1, 1 << 20])
+def test_rows_without_a_page_are_not_read_back(entry):
+    """A table entry that names no page: its rows are absent, and their outputs
+    stay as they were."""
+    d, P, n = 64, 16, 50
+    c = Cache(1, 6, P, 4, 1, 2, d).fill([n], shuffle=4).random_rows(3)
+    c.pages.table[0, 1] = entry
+    out = [torch.full((1, 1, 2, n, d), 7.0, dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    st = new_status()
+    R.kv_expand_q4(c.pool, c.pages, *out, status=st)
+    assert st.item() == R.STATUS_BAD_INDEX
+    for h in range(2):
+        for o, want in zip(out, c.rows(0, 0, h)):
+            want = torch.from_numpy(want).float().bfloat16()
+            want[P:2 * P] = 7.0
+            assert torch.equal(o[0, 0, h].cpu(), want)
