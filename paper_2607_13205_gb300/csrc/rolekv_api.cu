@@ -1092,8 +1092,8 @@ int fill_paged(const rolekv_pages* pg, const rolekv_pool* pool, const int32_t* s
       (pool->L > 1 && pool->s_layer < page))
     return fail(ROLEKV_ERR_INVALID_ARG, "pool strides must be multiples of 16 bytes, at least a page's %lld",
                 static_cast<long long>(page));
-  if (static_cast<int64_t>(pool->L) * b * pool->Hkv > INT32_MAX / 512)
-    return fail(ROLEKV_ERR_UNSUPPORTED, "too many units");
+  if (static_cast<int64_t>(pool->L) * pool->Hkv > INT32_MAX / 512)
+    return fail(ROLEKV_ERR_UNSUPPORTED, "too many layers and heads");
   a->pool = static_cast<uint8_t*>(pool->ptr);
   a->s_layer = pool->s_layer;
   a->s_page = pool->s_page;
@@ -1116,8 +1116,10 @@ bool overlap(const int32_t* x, int64_t nx, const int32_t* y, int64_t ny) {
   return x0 < y0 + static_cast<uintptr_t>(ny) * 4 && y0 < x0 + static_cast<uintptr_t>(nx) * 4;
 }
 
-// One call's grid: `per` CTAs or warps for each unit.
+// One call's units, and its grid: a warp or more for each eight rows of a unit.
 int check_grid(const PagedArgs& a, int64_t rows) {
+  if (static_cast<int64_t>(a.L) * a.b * a.Hkv > INT32_MAX / 512)
+    return fail(ROLEKV_ERR_UNSUPPORTED, "too many units");
   if (static_cast<int64_t>(a.L) * a.b * a.Hkv * ((rows + 7) / 8) > INT32_MAX)
     return fail(ROLEKV_ERR_UNSUPPORTED, "too many rows in one call");
   return ROLEKV_OK;

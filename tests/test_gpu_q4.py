@@ -1068,3 +1068,39 @@ def test_rows_without_a_page_are_not_read_back(entry):
             want = torch.from_numpy(want).float().bfloat16()
             want[P:2 * P] = 7.0
             assert torch.equal(o[0, 0, h].cpu(), want)
+
+
+def test_a_book_of_more_slots_than_a_batch_takes():
+    """Tens of thousands of slots of a pool of many layers and heads, a few of
+    them in use: room made, pages shared and copied, pages moved."""
+    L, Hkv, d, P, n_seqs = 32, 8, 64, 16, 20000
+    c = Cache(n_seqs, 12, P, 2, L, Hkv, d, seed=1)
+    use = [3, 1500, 19999]
+    for i, s in enumerate(use):
+        c.book.lens[s], c.book.table[s][0], c.book.refs[2 * i + 4] = 7 + i, 2 * i + 4, 1
+    c.upload()
+    parent = list(range(n_seqs))
+    parent[17000] = 1500
+    c.book.fork(parent)
+    R.kv_pages_fork(c.pages, i32(parent))
+    c.check_book()
+    add, pos, st = [0] * n_seqs, torch.full((n_seqs,), 9, dtype=torch.int32, device=DEV), new_status()
+    for s in (3, 1500, 17000):
+        add[s] = 10
+    R.kv_pages_reserve(c.pages, c.pool, i32(add), pos, status=st)
+    want, copies = c.book.reserve(add)
+    for src, dst, rows in copies:
+        recs = -(-rows // 16)
+        c.want[:, dst, :, :recs] = c.want[:, src, :, :recs]
+    assert pos.tolist() == want and st.item() == 0
+    c.check_book()
+    c.check_pool()
+    live = torch.zeros(1, dtype=torch.int32, device=DEV)
+    R.kv_pages_pack(c.pages, c.pool, n_live=live)
+    n, moves = c.book.pack()
+    for src, dst in moves:
+        c.want[:, dst] = c.want[:, src]
+    assert live.item() == n and len(moves) > 0
+    c.check_book()
+    got = c.pool.cpu().numpy()
+    assert np.array_equal(got[:, :n], c.want[:, :n])

@@ -336,3 +336,12 @@ def test_decode_refuses_more_rows_than_it_counts(lib):
     assert go(64) == WS                       # (2^31 - 2^13 pieces: the next check, of the workspace, fails)
     assert go(65) == UNS
     assert go(64, Hkv=60000) == UNS           # (more of them than 2^31 a CTA)
+
+
+def test_books_of_many_slots_are_taken(lib):
+    """Slots times layers and heads are no batch: the next check, of the
+    workspace, is the one that fails."""
+    pages, pool = _pages(n_seqs=20000), _pool(L=32, Hkv=8, s_page=8 * 2 * 2304, s_layer=20 * 8 * 2 * 2304)
+    for call in ("reserve", "pack"):
+        assert _calls(lib, pages, pool, ws=None, ws_bytes=0)[call]() == WS
+    assert _calls(lib, pages, pool, b=20000)["append"]() == UNS         # (that is one)
