@@ -429,14 +429,15 @@ int kv_pages_reserve(const rolekv_pages* pages, const rolekv_pool* pool, const i
  * holds and takes over the pages and the length that slot parent[x] (device
  * int32 [n_seqs]) had before the call; parent[x] = x leaves it as it is,
  * parent[x] = -1 empties it.  No row is copied: see kv_pages_reserve.  Another
- * value leaves the slot as it is and sets ROLEKV_STATUS_BAD_INDEX. */
+ * value leaves the slot as it is and sets ROLEKV_STATUS_BAD_INDEX.  parent and
+ * the tables do not overlap. */
 int kv_pages_fork(const rolekv_pages* pages, const int32_t* parent, void* workspace, size_t workspace_bytes,
                   int32_t* status_dev, void* stream);
 
 /* The pages in use moved to the front of the pool: afterwards pages 0 ..
- * *n_live - 1 are in use and the others free (n_live: optional device int32).
- * Pages behind the new end move, in ascending order, into the free ones before
- * it, in ascending order; the tables follow. */
+ * *n_live - 1 are in use and the others free (n_live: optional device int32,
+ * outside the tables).  Pages behind the new end move, in ascending order, into
+ * the free ones before it, in ascending order; the tables follow. */
 int kv_pages_pack(const rolekv_pages* pages, const rolekv_pool* pool, int32_t* n_live, void* workspace,
                   size_t workspace_bytes, int32_t* status_dev, void* stream);
 

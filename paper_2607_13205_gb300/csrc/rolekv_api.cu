@@ -1116,6 +1116,12 @@ bool overlap(const int32_t* x, int64_t nx, const int32_t* y, int64_t ny) {
   return x0 < y0 + static_cast<uintptr_t>(ny) * 4 && y0 < x0 + static_cast<uintptr_t>(nx) * 4;
 }
 
+// Does an int32 array share an element with the tables?
+bool overlaps_tables(const int32_t* x, int64_t n, const rolekv_pages& pg) {
+  const int64_t ns = pg.n_seqs;
+  return overlap(x, n, pg.table, ns * pg.max_pages) || overlap(x, n, pg.lens, ns) || overlap(x, n, pg.refs, pg.n_pages);
+}
+
 // One call's units, and its grid: a warp or more for each eight rows of a unit.
 int check_grid(const PagedArgs& a, int64_t rows) {
   if (static_cast<int64_t>(a.L) * a.b * a.Hkv > INT32_MAX / 512)
@@ -1173,8 +1179,7 @@ int kv_pages_reserve(const rolekv_pages* pages, const rolekv_pool* pool, const i
   if (rc) return rc;
   if ((rc = check_int_array("add", add, true)) || (rc = check_int_array("pos", pos, true))) return rc;
   const int64_t ns = pages->n_seqs;
-  if (overlap(pos, ns, add, ns) || overlap(pos, ns, pages->lens, ns) || overlap(add, ns, pages->lens, ns) ||
-      overlap(pos, ns, pages->table, ns * pages->max_pages) || overlap(pos, ns, pages->refs, pages->n_pages))
+  if (overlap(pos, ns, add, ns) || overlaps_tables(add, ns, *pages) || overlaps_tables(pos, ns, *pages))
     return fail(ROLEKV_ERR_INVALID_ARG, "add, pos and the tables are arrays of their own");
   a.add = add;
   a.pos = pos;
@@ -1192,6 +1197,8 @@ int kv_pages_fork(const rolekv_pages* pages, const int32_t* parent, void* worksp
   int rc = fill_pages(pages, nullptr, workspace, workspace_bytes, status_dev, &a);
   if (rc) return rc;
   if ((rc = check_int_array("parent", parent, true))) return rc;
+  if (overlaps_tables(parent, pages->n_seqs, *pages))
+    return fail(ROLEKV_ERR_INVALID_ARG, "parent and the tables are arrays of their own");
   a.parent = parent;
   stage_begin();
   const cudaError_t e = launch_pages_fork(a, static_cast<cudaStream_t>(stream));
@@ -1208,6 +1215,8 @@ int kv_pages_pack(const rolekv_pages* pages, const rolekv_pool* pool, int32_t* n
   int rc = fill_pages(pages, pool, workspace, workspace_bytes, status_dev, &a);
   if (rc) return rc;
   if ((rc = check_int_array("n_live", n_live, false))) return rc;
+  if (n_live != nullptr && overlaps_tables(n_live, 1, *pages))
+    return fail(ROLEKV_ERR_INVALID_ARG, "n_live lies in the tables");
   a.n_live = n_live;
   stage_begin();
   const cudaError_t e = launch_pages_pack(a, static_cast<cudaStream_t>(stream));

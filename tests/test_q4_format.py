@@ -345,3 +345,14 @@ def test_books_of_many_slots_are_taken(lib):
     for call in ("reserve", "pack"):
         assert _calls(lib, pages, pool, ws=None, ws_bytes=0)[call]() == WS
     assert _calls(lib, pages, pool, b=20000)["append"]() == UNS         # (that is one)
+
+
+def test_calls_refuse_arrays_that_are_their_tables(lib):
+    """add, parent and n_live inside an array that the call writes."""
+    pages, pool = _pages(table=1 << 20, lens=1 << 21, refs=1 << 22), _pool()
+    p = ctypes.c_void_p
+    for at in (1 << 20, (1 << 20) + 4 * 31, (1 << 20) - 12, 1 << 21, (1 << 21) + 12, 1 << 22, (1 << 22) + 76):
+        assert lib.kv_pages_reserve(_ref(pages), _ref(pool), p(at), p(1 << 24), FAKE, BIG, None, None) == INV, hex(at)
+        assert lib.kv_pages_fork(_ref(pages), p(at), FAKE, BIG, None, None) == INV, hex(at)
+    for at in (1 << 20, (1 << 20) + 4 * 31, 1 << 21, (1 << 21) + 12, 1 << 22, (1 << 22) + 76):
+        assert lib.kv_pages_pack(_ref(pages), _ref(pool), p(at), FAKE, BIG, None, None) == INV, hex(at)
