@@ -58,6 +58,29 @@ def write_row(rec: np.ndarray, row: int, k, v, empty: bool = False):
             rec[at] = (int(rec[at]) & ~(15 << sh) & 255) | ((int(code[e]) + 8) << sh)
 
 
+def write_rows(recs: np.ndarray, rec: np.ndarray, row: np.ndarray, k: np.ndarray, v: np.ndarray, empty=None):
+    """write_row for many at once: row[i] of the record recs[rec[i]] (uint8
+    [records][18 d], no place twice) from fp64 rows k[i], v[i] [d]."""
+    n, d = k.shape
+    J = d // 32
+    none = np.zeros(n, bool) if empty is None else np.asarray(empty, bool)
+    rec, row = np.asarray(rec)[:, None], np.asarray(row)[:, None]
+    e = np.arange(0, d, 2)[None]                                  # a byte: elements e and e + 1
+    j, w = e // 32, e % 32
+    for x, c0, s0, is_v in ((k, 0, 16 * d, False), (v, 8 * d, 17 * d, True)):
+        code, s = quantise(np.where(none[:, None], 0.0, x))
+        bits = scale_bits(s)
+        if not is_v:
+            bits[none] = 0x8000
+        for i in range(2):
+            recs[rec, s0 + 2 * (row * J + np.arange(J)[None]) + i] = (bits >> (8 * i)).astype(np.uint8)
+        if is_v:
+            word, byte = ((row // 8) * 32 + (w // 4) * 4 + (row % 8) // 2) * J + j, (row % 2) * 2 + w % 4 // 2
+        else:
+            word, byte = ((row // 8) * 32 + (row % 8) * 4 + w // 8) * J + j, w % 8 // 2
+        recs[rec, c0 + 4 * word + byte] = (code[:, 0::2] + 8) | ((code[:, 1::2] + 8) << 4)
+
+
 def read_row(rec: np.ndarray, row: int):
     """(k, v, empty) of a record's row, fp64."""
     d = rec.size // 18

@@ -917,7 +917,7 @@ def test_a_part_of_no_weight_keeps_its_nan(seqs, where):
     R.decode_attention_q4(q.to(DEV), c.pool, c.pages, out)
     got = out.cpu()
     if where == "keys":
-        assert torch.isnan(got).all(), f"{int(torch.isfinite(got).any(-1).sum())} heads of {got.shape[2] * seqs} are finite"
+        assert torch.isnan(got).all(), f"{int(torch.isfinite(got).any(-1).sum())} heads are finite"
     else:
         assert torch.isnan(got[..., :32]).all(), "a NaN value does not show"
         assert torch.isfinite(got[..., 32:]).all()
@@ -1104,3 +1104,130 @@ def test_a_book_of_more_slots_than_a_batch_takes():
     c.check_book()
     got = c.pool.cpu().numpy()
     assert np.array_equal(got[:, :n], c.want[:, :n])
+
+
+@pytest.mark.parametrize("more", [0, 1])
+def test_attention_around_the_choice_of_join_on_this_device(more):
+    """As many units as are joined one by one, a unit to four CTAs, and one more."""
+    d, P, n = 64, 64, 900
+    units = 3 * sms() // 4 + more
+    c = Cache(units, units * 15, P, 15, 1, 1, d).fill([n if s % 7 else 0 for s in range(units)], shuffle=2)
+    k, v = (bf16((1, units, 1, n, d), x).to(DEV) for x in (1, 2))
+    R.kv_append_q4(c.pool, c.pages, k, v, i32([0 if s % 7 else -1 for s in range(units)]))
+    c.want = c.pool.cpu().numpy()
+    q = bf16((1, units, 2, d), 9)
+    out = torch.full((1, units, 2, d), 7.0, device=DEV)
+    R.decode_attention_q4(q.to(DEV), c.pool, c.pages, out)
+    check_attention(out, q, c)
+
+
+def store_waves(units, items):
+    """Waves of the SMs' 32 warps that a call of so many items has."""
+    return units * items / (32 * sms())
+
+
+def kept_of(rng, n, m):
+    """m ascending positions of n tokens, every eighth an empty slot."""
+    x = np.sort(rng.permutation(n)[:m])
+    x[rng.random(x.size) < 0.125] = -1
+    return x
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("above", [False, True])
+@pytest.mark.parametrize("packed", [False, True])
+def test_compact_around_the_choice_of_items_a_warp(d, above, packed):
+    """Calls just below and from so many warps on that each takes several items
+    one after another (six waves of them): every row's bytes, and nothing else,
+    at every place in a record, with items that are no multiple of a warp's, and
+    in the packed batch with sequences without tokens and of very different
+    lengths."""
+    Hkv, L, P, budget = 4, 1, 48, 0.5
+    rng = np.random.default_rng(d + above)
+    if packed:
+        lens = [0, 1, 1200, 3] + [int(x) for x in rng.integers(0, 60, 12)]
+    else:
+        lens = [36]
+    top = R.kept_rows(max(lens), budget)
+    items = ((top + 14) // 16 + 1) * (2 if d == 128 else 1)
+    assert packed or items % 4 != 0
+    b = -(-6 * 32 * sms() // (items * Hkv)) - (0 if above else 1)
+    assert (store_waves(b * Hkv, items) >= 6) == above
+    if packed:
+        lens += [int(x) for x in rng.integers(0, 60, b - len(lens))]
+    else:
+        lens = lens * b
+    assert len(lens) == b
+    kept = [R.kept_rows(n, budget) for n in lens]
+    pos = [int(x) for x in rng.integers(0, 40, b)]
+    pos[0:3] = [0, 15, 8]
+    rows = [p + m for p, m in zip(pos, kept)]
+    c = Cache(b, pages_for(rows, P), P, -(-max(rows) // P), L, Hkv, d, seed=1).fill(rows, shuffle=3)
+    T = sum(lens)
+    k, v = bf16((L, T, Hkv, d), 1), bf16((L, T, Hkv, d), 2, 3.0)      # (token rows, also of the dense batch)
+    batch = R.Batch(L, b, Hkv, Hkv, d, max(lens), seqlens=lens if packed else None)
+    if packed:
+        kd, vd = k.to(DEV), v.to(DEV)
+    else:
+        kd, vd = (x.view(L, b, 36, Hkv, d).transpose(2, 3).to(DEV) for x in (k, v))
+    at = np.cumsum([0] + lens)
+    idx = [[kept_of(rng, n, m) for n, m in zip(lens, kept)] for _ in range(Hkv)]
+    if packed:
+        keep = np.stack([np.concatenate(x) for x in idx])[None]
+    else:
+        keep = np.stack([np.stack(x) for x in idx], 1)[None]          # [L][b][Hkv][K]
+    k64, v64 = f64(k)[0], f64(v)[0]
+    for h in range(Hkv):
+        j = np.concatenate([np.arange(m) for m in kept])
+        s = np.repeat(np.arange(b), kept)
+        t = np.concatenate(idx[h])
+        token = at[s] + np.maximum(t, 0)
+        row = np.asarray(pos)[s] + j
+        page = np.asarray(c.book.table)[s, row // P]
+        recs = c.want[0].reshape(-1, 18 * d)
+        Q.write_rows(recs, (page * Hkv + h) * (P // 16) + row % P // 16, row % 16, k64[token, h], v64[token, h], t < 0)
+    st = new_status()
+    R.kv_compact_q4(batch, kd, vd, torch.from_numpy(keep).int().to(DEV), budget, c.pool, c.pages, i32(pos), status=st)
+    c.check_pool()
+    assert st.item() == 0
+
+
+@pytest.mark.parametrize("form", ["rows", "rows of four heads", "records"])
+def test_every_mantissa_and_group_maximum(form):
+    """Every 8-bit mantissa of an element with every one of its group's largest
+    element, at each exponent that gives a code of its own, both signs, half-way
+    quotients among them, and at scales about 2^-126 and of the largest: the
+    oracle's bytes from each of the storing kernels."""
+    d = 128
+    rows = []
+    for e in (0, 120, -131):
+        m = np.arange(128, 256)
+        x = np.concatenate([np.ldexp(np.arange(128.0, 256.0), -i) for i in range(7)])  # 896 for each maximum
+        x = np.concatenate([x, np.zeros(-x.size % 31)]).reshape(-1, 31)
+        g = np.concatenate([np.broadcast_to(m[:, None, None], (128, x.shape[0], 1)),
+                            np.broadcast_to(x[None], (128,) + x.shape)], -1)
+        g = np.where(np.abs(g) <= g[..., :1], g, 0.0).reshape(-1, 32)
+        g[1::2] *= -1.0
+        rows.append(np.ldexp(g[:g.shape[0] // 4 * 4].reshape(-1, d), e))
+    x = torch.from_numpy(np.concatenate(rows)).bfloat16()
+    n = x.shape[0]
+    k, v = f64(x), f64(x.flip(1))
+    vd = x.flip(1)
+    if form == "records":
+        P = 1024
+        c = Cache(1, -(-n // P), P, -(-n // P), 1, 1, d).fill([n])
+        R.kv_append_q4(c.pool, c.pages, x.to(DEV).view(1, 1, 1, n, d), vd.to(DEV).view(1, 1, 1, n, d), i32([0]))
+        page, row, heads = np.arange(n) // P, np.arange(n) % P, 1
+    else:
+        P, heads = 16, 1 if form == "rows" else 4
+        L = 1 if heads == 1 else -(-2 * 32 * sms() // (n * heads))
+        assert (store_waves(L * n * heads, 1) >= 2) == (heads > 1)
+        c = Cache(n, n, P, 1, L, heads, d).fill([16] * n)
+        kd, vv = (y.to(DEV).view(1, n, 1, 1, d).expand(L, n, heads, 1, d).contiguous() for y in (x, vd))
+        R.kv_append_q4(c.pool, c.pages, kd, vv, i32([s % 16 for s in range(n)]))
+        page, row = np.arange(n), np.arange(n) % 16
+    for l in range(c.want.shape[0]):
+        for h in range(heads):
+            recs = c.want[l].reshape(-1, 18 * d)
+            Q.write_rows(recs, (page * heads + h) * (P // 16) + row // 16, row % 16, k, v)
+    c.check_pool()

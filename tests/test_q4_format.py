@@ -356,3 +356,65 @@ def test_calls_refuse_arrays_that_are_their_tables(lib):
         assert lib.kv_pages_fork(_ref(pages), p(at), FAKE, BIG, None, None) == INV, hex(at)
     for at in (1 << 20, (1 << 20) + 4 * 31, 1 << 21, (1 << 21) + 12, 1 << 22, (1 << 22) + 76):
         assert lib.kv_pages_pack(_ref(pages), _ref(pool), p(at), FAKE, BIG, None, None) == INV, hex(at)
+
+
+def test_rows_written_at_once():
+    """The oracle's two ways to write rows are the same."""
+    for d in (64, 128):
+        rng = np.random.default_rng(d)
+        g = torch.Generator().manual_seed(d)
+        k, v = (torch.randn(40, d, generator=g).bfloat16().double().numpy() for _ in "kv")
+        k[3, 5], v[4, 40] = np.inf, np.nan
+        place = rng.permutation(5 * 16)[:40]
+        empty = rng.random(40) < 0.2
+        want = rng.integers(0, 256, (5, 18 * d)).astype(np.uint8)
+        got = want.copy()
+        for i in range(40):
+            Q.write_row(want[place[i] // 16], int(place[i] % 16), k[i], v[i], bool(empty[i]))
+        Q.write_rows(got, place // 16, place % 16, k, v, empty)
+        assert np.array_equal(got, want)
+
+
+def _bf16(x32):
+    """fp32 to bf16 bits, ties to even."""
+    u = x32.view(np.uint32)
+    return ((u + 0x7FFF + ((u >> 16) & 1)) >> 16).astype(np.uint16)
+
+
+def test_scale_by_a_product_over_all_maxima():
+    """The kernels take m / 7 as a product with fp32's 1/7, rounded to fp32 and
+    then to bf16, and 0 where that is below 2^-126: the exact quotient's scale for
+    every finite bf16 m."""
+    m = (np.arange(0x7F80, dtype=np.uint32) << 16).view(np.float32)
+    bits = _bf16(m * (np.float32(1) / np.float32(7)))
+    bits[bits < 0x0080] = 0
+    _, s = Q.quantise(np.repeat(m.astype(np.float64)[:, None], 32, 1))
+    assert np.array_equal(bits, Q.scale_bits(s[:, 0]))
+
+
+@pytest.mark.parametrize("off", [-1, 0, 1])
+@pytest.mark.parametrize("form", ["nibble", "byte"])
+def test_codes_with_an_approximate_reciprocal(form, off):
+    """Both of the kernels' forms of floor(x / s + 1/2) + 8, one fused
+    multiply-add each, with a reciprocal that is one unit in the last place off
+    (as much as the approximate instruction may be): the exact quotient's code
+    for every pair of 8-bit mantissas, ties among them."""
+    a, b = np.meshgrid(np.arange(128, 256), np.arange(128, 256), indexing="ij")
+    ties = 0
+    s32 = b.astype(np.float32)
+    inv = ((np.float32(1) / s32).view(np.uint32) + np.uint32(off & 0xFFFFFFFF)).view(np.float32).astype(np.float64)
+    for k in range(-12, 4):
+        for sign in (1, -1):
+            x = sign * np.ldexp(a.astype(np.float64), k)
+            ok = np.abs(x) <= 7.0 * (1 + 2.0 ** -8) * b
+            if form == "nibble":
+                t = (x * inv + (8.0 + 2.0 ** -14)).astype(np.float32)          # (exact in fp64, one rounding: the fma)
+                n = (t + np.float32(8388608.0)).view(np.uint32) & 15
+            else:
+                t = (x * inv + (136.5 + 2.0 ** -14)).astype(np.float32)
+                n = (t.view(np.uint32) >> 16) & 255
+            num = 2 * sign * a * 2 ** (k + 12) + b * 2 ** 12        # 2^12 (2 x + s) over 2^13 s, whole numbers
+            want = num // (b * 2 ** 13) + 8
+            assert np.array_equal(n[ok], want[ok])
+            ties += int((num[ok] % (b * 2 ** 13)[ok] == 0).sum())
+    assert ties > 100
