@@ -16,7 +16,8 @@
 // is the operands' order in registers, see q4_format.h).  A code becomes an
 // operand in two steps: a mask that also sets the exponent gives 1024 + code
 // (nibbles 0, 4 of a word) or 1024 + 16 code (nibbles 1, 5), and an fp16 addition
-// takes the 1024 and the offset of 8 off, exactly.  (Left as subnormal numbers,
+// takes the 1024 and the offset of 8 off, exactly (a published way to turn whole
+// numbers into floating point; the factor of 16 goes into q and the outputs).  (Left as subnormal numbers,
 // code * 2^-24, they would cost the mask alone, but the tensor cores align a
 // product's bits by its operands' exponents, and sums came out with 17 bits.)
 //   S = K Q^T   16 rows x heads.  q is scaled by a power of two to below 2^15,
@@ -37,14 +38,17 @@
 //     the product, 1% of the time): beside large logits fp32 has no room for it,
 //     and the probabilities' sums would span more powers of two than fp32 has.
 //     A warp's sums leave it as means, the power taken off.
-// What bounds it is instructions: some 390 a record and warp, of which about 145
-// make operands of codes, issued 0.6 a cycle and scheduler with the ALU pipe at
-// 46%, FMA 39%, tensor 30%, DRAM 49%.  131072 rows of 8 heads, 151 MB: 45 us,
-// 3.4 TB/s.  An uneven batch, 600 MB: 157 us, 3.8 TB/s.  (All of a piece's work
-// but one read left out, it took 106 us of the 152 before records were summed
-// apart; the copies left out instead, 147 of 160 before there was a fifth warp.)
-// Three CTAs an SM at 128 registers a thread; two take 224 us.  Records one by
-// one, which fit four, took 162 where two by two took 157.
+// What bounds it is issue that stalls: some 390 instructions a record and warp, of
+// which about 145 make operands of codes, at 0.61 a cycle and scheduler, with no
+// pipe above half (ALU 46%, FMA 40%, tensor 30%, DRAM 49%).  Without a gap they
+// would take 81 us of an uneven batch's 158 (600 MB, 3.8 TB/s; its bytes alone 88).
+// A scheduler's three warps wait for results of fixed latency (1.4 cycles an
+// instruction), for one another (0.85) and for bursts on the math pipes (0.7), and
+// hardly for copies (0.5).  131072 rows of 8 heads, 151 MB: 45 us, 3.4 TB/s.  (All
+// of a piece's work but one read left out, the batch took 106 us of the 152 before
+// records were summed apart; the copies left out instead, 147 of 160 before there
+// was a fifth warp.)  Three CTAs an SM at 128 registers a thread; two take 224 us.
+// Records one by one, which fit four, took 162 where two by two took 157.
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
@@ -73,10 +77,12 @@ constexpr int kTurn = 12;           // floats of a row of probabilities (eight, 
 // join listed by CTA or, for few units of many parts, by unit; or a unit to each.
 enum { kShared = 0, kFewUnits = 1, kOneUnit = 2 };
 // Units of so many pieces at most go to a CTA each: no parts, no second launch.
-// Shared against whole, us, by rows of a unit:  128: 7.0, 5.8   256: 7.6, 6.8
-// 384: 7.8, 7.6   512: 7.9, 8.4 (2 units);  128: 9.3, 6.6   256: 11.1, 7.9
-// 384: 14.6, 9.2 (256 units);  128: 52, 60   256: 73, 80   384: 89, 94 (4096);
-// 128: 289, 247   256: 382, 306   384: 442, 364 (16384).
+// Shared against whole, us, by rows of a unit of 8 heads:  128: 7.1, 5.6   256:
+// 8.4, 6.6   384: 8.6, 7.4   512: 8.6, 8.4 (2 units);  128: 9.1, 6.4   256: 11.0,
+// 7.8   384: 15.3, 9.2   512: 17.7, 10.5 (256);  128: 51, 60   256: 73, 78   384:
+// 89, 94 (512 sequences);  128: 294, 245   256: 388, 304   384: 479, 363 (2048
+// sequences);  128: 183, 240   256: 247, 301   384: 312, 360 (64 sequences of 32
+// layers, where whole units cost a quarter).
 constexpr int kWholePieces = 12;
 
 template <int D>
@@ -236,14 +242,15 @@ __device__ __forceinline__ void next_unit(const Span& sp, Place* p) {
   p->end += sp.cum[p->s + 1] - sp.cum[p->s];
 }
 
-// What the warps of a CTA work on: kept in shared memory, out of the way of the
-// loop over the rows.
+// The four warps of a CTA that work on the rows meet.
 __device__ __forceinline__ void sync_consumers() {
   asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
 }
 // After a wait has run out, how long copies in flight are given to land.
 constexpr uint64_t kDrainNs = 50000000ull;
 
+// What they work on: kept in shared memory, out of the way of the loop over the
+// rows.
 struct Work {
   Place unit;
   int64_t x, end;                 // its pieces in this CTA's run
@@ -657,10 +664,11 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
           mma_f16(c1, a1, bh[0], bh[1], c1);
 #pragma unroll
           for (int k = 0; k < 4; k += 2) {
-            const float2 x0 = __fadd2_rn(make_float2(acc[2 * j][k], acc[2 * j][k + 1]), make_float2(c0[k], c0[k + 1]));
-            const float2 x1 = __fadd2_rn(make_float2(acc[2 * j + 1][k], acc[2 * j + 1][k + 1]), make_float2(c1[k], c1[k + 1]));
-            acc[2 * j][k] = x0.x, acc[2 * j][k + 1] = x0.y;
-            acc[2 * j + 1][k] = x1.x, acc[2 * j + 1][k + 1] = x1.y;
+            float *s0 = acc[2 * j] + k, *s1 = acc[2 * j + 1] + k;
+            const float2 x0 = __fadd2_rn(make_float2(s0[0], s0[1]), make_float2(c0[k], c0[k + 1]));
+            const float2 x1 = __fadd2_rn(make_float2(s1[0], s1[1]), make_float2(c1[k], c1[k + 1]));
+            s0[0] = x0.x, s0[1] = x0.y;
+            s1[0] = x1.x, s1[1] = x1.y;
           }
         }
       }
@@ -769,8 +777,8 @@ __global__ void __launch_bounds__(kBlock, kQ4DecodeCtasPerSm) q4_decode_kernel(c
 // parts.  Lanes run over the elements.  (8 units of 57 parts: 13 us with all
 // heads in one CTA, 9 with one each, both from cold caches.)  Few means at most
 // one unit to four CTAs.  By CTA against by (unit, head), 8192 rows a unit, us for
-// the whole call:  8 units: 14.0, 11.7   32: 20.5, 19.2   112: 41.3, 41.0
-// 128: 47.8, 48.7   256: 80.9, 84.0.
+// the whole call:  8 units: 16.2, 13.3   32: 22.3, 20.6   64: 28.9, 28.2   112:
+// 41.9, 41.7   128: 48.7, 48.5   256: 81.8, 83.8.
 template <int D, bool kFew>
 __global__ void __launch_bounds__(kJoinWarps * 32) q4_join_kernel(const Q4DecodeArgs a) {
   constexpr int E = D / 32;

@@ -2,10 +2,14 @@
 // compaction of Section 6, with four bits an element) and new tokens' rows are
 // quantised into pages, and rows are read back as bf16.  Memory-bound: a row's
 // 4 d bytes of K and V and its 9 d / 8 bytes in the cache move once.  839 thousand
-// kept rows of 128 elements, 550 MB: compaction 96 us (5.8 TB/s), reading back 84
-// (6.5 TB/s, near the copy rate).  An uneven packed batch of 1.45 million,
-// 953 MB: compaction 173 us (5.5 TB/s), reading back 145 (6.6).  What bounds compaction is
-// instructions: 0.66 issued a cycle and scheduler, the ALU pipe at 54%, DRAM at 64%.
+// kept rows of 128 elements, 550 MB: compaction 95 us (5.8 TB/s), reading back 83
+// (6.6 TB/s, near the copy rate).  An uneven packed batch of 1.45 million, 953 MB:
+// compaction 173 us (5.5 TB/s), reading back 143 (6.7).  What bounds compaction is
+// instructions: 0.66 issued a cycle and scheduler, the ALU pipe at 54%, DRAM at 67%.
+// Single new rows cost more than their bytes: a row's V codes are 16-bit halves of
+// words that two rows share, 64 bytes of them in eight sectors, which is the price
+// of an order that attention reads without exchanging anything.  65536 rows, 43 MB:
+// 17.9 us, where the copy rate would take 6.3.
 // Both, of the first, step by step: a warp a row, with two-byte stores, 718 us; a
 // warp a whole record of 128 elements 199; half a record (64 registers, 32 warps an
 // SM) 191; indexes divided by products 181.

@@ -556,7 +556,7 @@ def kv_compact_q4(batch: Batch, k: torch.Tensor, v: torch.Tensor, keep_idx: torc
     dev = pool.get_device()
     for t in (k, v):
         if t.get_device() != dev and not (t.device.type == "cpu" and t.is_pinned()):
-            raise ValueError(f"k or v on {t.device}: neither on the current device, cuda:{dev}, nor in pinned host memory")
+            raise ValueError(f"k or v on {t.device}: not on the current device, cuda:{dev}, nor in pinned host memory")
     _check(lib().kv_compact_q4(ctypes.byref(batch.desc), _rows_desc(batch, k, "k"), _rows_desc(batch, v, "v"),
                                _int32(keep_idx, batch.L * batch.Hkv * max(0, batch.kept_total(budget)), "keep_idx"),
                                budget, ctypes.byref(pool_desc(pool, pages)),
