@@ -798,6 +798,12 @@ __global__ void __launch_bounds__(kJoinWarps * 32) q4_join_kernel(const Q4Decode
 #pragma unroll
   for (int k = 0; k < E; ++k) o[k] = 0.f;
   if (hd < G) {
+    // (this warp's first part, on its way while the parts' weights are added: 0.6 us
+    // of a short layer's 15.7)
+    const int i0 = warp % W;
+    float first[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) first[k] = i0 < jn.z ? part(i0)[lane + 32 * k] : 0.f;
     // the parts' largest reference and, by it, the sum of all probabilities
     float M = -INFINITY, L = 0.f;
     const auto add = [&](float m, float l) {
@@ -813,11 +819,19 @@ __global__ void __launch_bounds__(kJoinWarps * 32) q4_join_kernel(const Q4Decode
       add(m, l);
     }
     const float by_all = L == 0.f ? 0.f : reciprocal(L);
+    // (parts without a row are zeros; a NaN shows whatever its part's weight)
+    const auto weight = [&](const float* p) {
+      return p[D] == -INFINITY ? 0.f : fast_exp2(p[D] - M) * p[D + 1] * by_all;
+    };
+    if (i0 < jn.z) {
+      const float f = weight(part(i0));
+#pragma unroll
+      for (int k = 0; k < E; ++k) o[k] = f * first[k];
+    }
 #pragma unroll 4
-    for (int i = warp % W; i < jn.z; i += W) {
+    for (int i = i0 + W; i < jn.z; i += W) {
       const float* p = part(i);
-      // (parts without a row are zeros; a NaN shows whatever its part's weight)
-      const float f = p[D] == -INFINITY ? 0.f : fast_exp2(p[D] - M) * p[D + 1] * by_all;
+      const float f = weight(p);
 #pragma unroll
       for (int k = 0; k < E; ++k) o[k] += f * p[lane + 32 * k];
     }
